@@ -367,7 +367,8 @@ int64_t dq_comm_cost_bits(int W, int64_t d, int b, int32_t n_norms, int B_pre);
  *            alignment beyond the element's.  Per-row arrays are [batch * rows], contiguous.
  *   tokens   the token that was taken in each row.  A row whose token is outside [0, vocab), e.g.
  *            -100, does not count: it is not read, its log-probability is 0 and its gradient zeros.
- *   logp     (z_y - m) / T - ln s, m = max_v z_v, s = sum_v exp((z_v - m) / T), T the temperature.
+ *   logp     (z_y - m) / T - ln s, m = max_v z_v, s = sum_v exp((z_v - m) / T), T the temperature
+ *            (from 4.3e-39 to 3.2e36; any other is refused: log2(e) / T is a binary32 factor).
  *            -inf logits have probability 0; a NaN or +inf, or a row of -inf alone, gives NaN.
  *   dlogits  (grad_scale * dL/dlogp / T) * ([v = y] - p_v), written in full, rounded once to the
  *            logits' type; the same type and sizes as the logits, strides of its own, rows apart.

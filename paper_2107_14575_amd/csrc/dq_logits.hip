@@ -16,6 +16,7 @@
 // (a copy of 2 GiB by torch: 4.9 TB/s).  The preference loss has to know all rows of a pair before the first gradient and reads twice.  Small calls are
 // their launches: 2.8 us each on the host, beside 1.6 to 3.3 for a call's arguments.
 #include <cmath>
+#include <limits>
 #include <type_traits>
 
 #include "dq_internal.h"
@@ -868,11 +869,13 @@ int gradient_of(const dq_logits_t* m, const dq_logits_t* logits, dq_rows& out)
 int64_t up(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 float exp2_scale(double temperature) { return static_cast<float>(1.4426950408889634 / temperature); } // log2(e) / T
-// the kernels' own factors have to be numbers of binary32
+// The kernels' own factors have to be numbers of binary32.  A difference of two logits may pass binary32 and is -inf then, which is right where its
+// exponential is 0 anyway: up to T = 3.27e36.  (Far beyond that the factor is 0, and its product with the -inf of a row's first maximum NaN.)
 bool usable(double temperature, double scale)
 {
-    return temperature > 0.0 && std::isfinite(temperature) && std::isfinite(scale) && std::isfinite(exp2_scale(temperature)) &&
-           std::isfinite(static_cast<float>(scale / temperature));
+    const float c = exp2_scale(temperature);
+    return temperature > 0.0 && std::isfinite(temperature) && std::isfinite(scale) && std::isfinite(c) &&
+           static_cast<double>(c) * std::numeric_limits<float>::max() >= 150.0 && std::isfinite(static_cast<float>(scale / temperature));
 }
 
 dim3 grid_of(int64_t workgroups)
