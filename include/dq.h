@@ -418,6 +418,7 @@ int dq_policy_loss(const dq_logits_t* logits, const int64_t* tokens_dev, double 
  * gradient); sequence p < pairs is preferred to sequence pairs + p.  With S_i the sum of a sequence's counted log-probabilities (average: their
  * mean; 0 for a sequence without any) and R_i = beta * (S_i - ref_logp_i):
  *     h = R_p - R_(pairs+p),  l = -(1 - label_smoothing) ln sigma(h) - label_smoothing ln sigma(-h),  L = (1/pairs) sum l
+ *   pairs         from 1 to 2^24
  *   seq_start_dev [2 * pairs + 1] int64;  ref_logp_dev [2 * pairs] or NULL (zeros)
  *   loss_dev      [4] float, written: L, the share of pairs with h > 0, the mean R of the preferred sequences, and of the others
  *   seq_logp_dev  [2 * pairs] float, written: S (under a reference model: what ref_logp_dev takes)

@@ -745,7 +745,8 @@ __global__ __launch_bounds__(THREADS) void k_preference_pairs(preference_args p,
     static_assert(WAVES == 4, "two wavefronts a sequence");
     __shared__ double sums[WAVES];
     __shared__ int counts[WAVES];
-    const int64_t pair = blockIdx.x;
+    const int64_t pair = workgroup();
+    if (pair >= p.pairs) return;
     const pair_rows rows(p, pair);
     const int wave = threadIdx.x / 64, mine = threadIdx.x / HALF, tid = threadIdx.x % HALF; // which sequence: 0 the preferred one
     const int64_t first = mine ? rows.first[1] : rows.first[0], end = mine ? rows.end[1] : rows.end[0];
@@ -774,7 +775,7 @@ __global__ __launch_bounds__(THREADS) void k_preference_pairs(preference_args p,
         term_sums{ { of_pair.loss, of_pair.h > 0.0 ? 1.0 : 0.0, of_pair.reward[0], of_pair.reward[1] } }.store(terms + pair);
         for (int k = 0; k < 2; ++k) seq_logp[rows.of[k]] = static_cast<float>(of_pair.total[k]);
     }
-    if (loss) sum_by_last(terms, blockIdx.x, gridDim.x, 1.0 / static_cast<double>(p.pairs), loss);
+    if (loss) sum_by_last(terms, static_cast<uint32_t>(pair), gridDim.x, 1.0 / static_cast<double>(p.pairs), loss);
 }
 
 // Few rows and few pairs: the forward pass's last workgroup to arrive does the pairs as well, a wavefront each, and there is one launch for two.  One pair of
@@ -1178,7 +1179,7 @@ extern "C" int dq_preference_loss(const dq_logits_t* logits, const int64_t* toke
     if (!preference_few(logits->dtype, a, p, seq_logp_dev, dlogp, loss_dev, stream)) {
         if (rows.count) forward(logits->dtype, a, reinterpret_cast<char*>(dlogp) + up(rows.count * 4), stream);
         const bool arrive = stream == nullptr && pairs <= MOST_ARRIVING;
-        hipLaunchKernelGGL(k_preference_pairs, dim3(static_cast<unsigned>(pairs)), dim3(THREADS), 0, stream, p, tokens_dev, logp, terms, seq_logp_dev, dlogp,
+        hipLaunchKernelGGL(k_preference_pairs, grid_of(pairs), dim3(THREADS), 0, stream, p, tokens_dev, logp, terms, seq_logp_dev, dlogp,
                            arrive ? loss_dev : nullptr);
         if (!arrive) sum_terms(terms, pairs, 1.0 / static_cast<double>(pairs), loss_dev, stream);
     }
