@@ -156,7 +156,8 @@ __device__ __forceinline__ bool last_to_arrive(uint32_t* counter, uint32_t n)
 
 __device__ __forceinline__ float log_probability(float of_token, const row_sum& all, double inv_t)
 {
-    return static_cast<float>(static_cast<double>(of_token - all.top) * inv_t - static_cast<double>(logf(all.sum)));
+    // the difference in binary64: in binary32 it overflows for logits at both ends of the type, where its product with a small 1 / T does not
+    return static_cast<float>((static_cast<double>(of_token) - static_cast<double>(all.top)) * inv_t - static_cast<double>(logf(all.sum)));
 }
 
 // adds the vectors first, first + step, ... below end of a row to `mine`.  STREAM: logits that nothing reads again; without it the last 256 MB of them stay in the

@@ -36,3 +36,31 @@ def test_the_most_pairs(dq, pairs):
     d = torch.cat([-g[0].expand(3), g[1].expand(4)])
     want, err = ref.dlogits(sm, d, scale=float(1 << 20), d_err=(0.25 * bound / pairs + 4 * U * d.abs()))
     ref.close(out, want, err)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("temperature", [1.0, 100.0, 1e20, 3.2e36])
+@pytest.mark.parametrize("vocab", [9, 700, 3000, 9000, 70000])
+def test_logits_at_both_ends_of_the_type(dq, dtype, temperature, vocab):
+    """z_y - m passes binary32 and (z_y - m) / T need not: -6.8e36 at T = 100, -6.8e18 at 1e20, and -213 at the largest temperature."""
+    ends = torch.finfo(dtype)
+    z, y, gen = make_logits(4, vocab, dtype, vocab)
+    for r in range(4):
+        z[r, (y[r] + 1) % vocab] = ends.max
+    z[0, y[0]] = ends.min
+    z[1, y[1]] = ends.min / 2
+    z[2] = ends.min
+    z[2, (y[2] + 1) % vocab] = ends.max
+    sm = ref.softmax(z, y, temperature)
+    want = sm["logp"].clone()
+    want[want < -ends.max] = -math.inf  # of binary32: its largest number is bfloat16's but for half a unit
+    if temperature > 1.0:
+        assert want.isfinite().all() and float(want[0]) < -200.0
+    logp, softmax = forward(dq, z.cuda(), y.cuda(), temperature)
+    ref.close(logp, want, torch.nan_to_num(sm["logp_err"], posinf=0.0))
+    ws = torch.empty(dq.policy_loss_workspace_bytes(4, vocab), dtype=torch.uint8, device="cuda")
+    loss, lp, out = torch.empty(4, device="cuda"), torch.empty(4, device="cuda"), torch.empty_like(z).cuda()
+    ones = torch.full((4,), 0.25, device="cuda")
+    dq.policy_loss(z.cuda(), y.cuda(), torch.zeros(4, device="cuda"), ones, ones, loss, lp, out, ws, temperature=temperature)
+    torch.cuda.synchronize()
+    ref.close(lp, want, torch.nan_to_num(sm["logp_err"], posinf=0.0))
