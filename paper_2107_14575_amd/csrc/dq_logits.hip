@@ -716,7 +716,8 @@ __device__ __forceinline__ pair_result pair_of(const preference_args& p, const d
     }
     const double h = r.reward[0] - r.reward[1], eps = p.smoothing;
     const double e = exp(-fabs(h)), rest = log1p(e); // -ln sigma(h) = rest + max(-h, 0)
-    const double loss = (1.0 - eps) * (rest + fmax(-h, 0.0)) + eps * (rest + fmax(h, 0.0));
+    // a sequence of probability 0 makes h infinite: the term whose factor is 0 is 0 then, not 0 times infinity
+    const double loss = (eps < 1.0 ? (1.0 - eps) * (rest + fmax(-h, 0.0)) : 0.0) + (eps > 0.0 ? eps * (rest + fmax(h, 0.0)) : 0.0);
     const double sigma = (h > 0.0 ? e : 1.0) / (1.0 + e); // of -h
     const double g = static_cast<double>(p.beta) * ((1.0 - eps) * sigma - eps * (1.0 - sigma)) / static_cast<double>(p.pairs);
     r.h = h;

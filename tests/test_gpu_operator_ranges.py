@@ -64,3 +64,43 @@ def test_logits_at_both_ends_of_the_type(dq, dtype, temperature, vocab):
     dq.policy_loss(z.cuda(), y.cuda(), torch.zeros(4, device="cuda"), ones, ones, loss, lp, out, ws, temperature=temperature)
     torch.cuda.synchronize()
     ref.close(lp, want, torch.nan_to_num(sm["logp_err"], posinf=0.0))
+
+
+@pytest.mark.parametrize("lens,vocab", [([3, 2, 4, 3], 60), ([70, 40, 50, 30], 9000)])
+@pytest.mark.parametrize("own_stream", [False, True])
+def test_sequences_of_probability_zero(dq, lens, vocab, own_stream):
+    """A token of probability 0 in one sequence of a pair: h is infinite, and a term of the loss whose factor is 0 adds nothing (-1 ln sigma(inf) - 0 ln sigma(-inf)
+    is 0).  The gradient is that of a sigmoid of 0 or 1."""
+    rows, pairs = sum(lens), 2
+    stream = torch.cuda.Stream() if own_stream else None
+    start = torch.tensor([0] + lens).cumsum(0)
+    for which, side in ((0, -math.inf), (2, math.inf)):  # the first pair's preferred sequence, or its other one
+        z, y, gen = make_logits(rows, vocab, torch.float32, 5)
+        row = int(start[which])
+        z[row, y[row]] = -math.inf
+        sm = ref.softmax(z, y)
+        S = torch.stack([sm["logp"][a:b].sum() for a, b in zip(start[:-1], start[1:])])
+        h1 = 0.5 * (S[1] - S[3])
+        sp = torch.nn.functional.softplus
+        for eps in (0.0, 0.25, 1.0):
+            # the first pair's loss: -ln sigma(h) has the factor 1 - eps, -ln sigma(-h) eps
+            infinite = (1 - eps if side < 0 else eps) > 0
+            l0 = math.inf if infinite else 0.0
+            want = torch.tensor([(l0 + float((1 - eps) * sp(-h1) + eps * sp(h1))) / 2])
+            g0 = (1 - eps) if side < 0 else -eps          # (1 - eps) sigma(-h) - eps sigma(h)
+            g1 = (1 - eps) * torch.sigmoid(-h1) - eps * torch.sigmoid(h1)
+            loss, seq = torch.full((4,), math.nan, device="cuda"), torch.full((4,), math.nan, device="cuda")
+            out = torch.full((rows, vocab), math.nan, device="cuda")
+            ws = torch.empty(dq.preference_loss_workspace_bytes(rows, vocab, pairs), dtype=torch.uint8, device="cuda")
+            torch.cuda.synchronize()
+            dq.preference_loss(z.cuda(), y.cuda(), start.cuda(), loss, seq, out, ws, beta=0.5, label_smoothing=eps, stream=stream)
+            torch.cuda.synchronize()
+            err = torch.nan_to_num(sm["logp_err"], posinf=0.0).sum() + 8 * U * S[S.isfinite()].abs().sum()
+            ref.close(loss[:1], want, (err + 4 * U) * (1 + want.abs().nan_to_num(posinf=0.0)))
+            assert float(loss[1]) == ((side > 0) + (float(h1) > 0)) / 2
+            assert float(seq[which]) == -math.inf and seq[[k for k in range(4) if k != which]].isfinite().all()
+            d = torch.zeros(rows, dtype=torch.float64)
+            for k, g in ((0, -g0), (1, -float(g1)), (2, g0), (3, float(g1))):
+                d[start[k]:start[k + 1]] = 0.5 * g / pairs
+            grad, bound = ref.dlogits(sm, d, d_err=err.expand(rows) * 0.25 + 4 * U)
+            ref.close(out, grad, torch.nan_to_num(bound))
