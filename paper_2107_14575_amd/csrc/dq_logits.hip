@@ -381,8 +381,13 @@ struct policy_scalars {
 __device__ __forceinline__ float4 policy_row(const policy_args& p, const policy_scalars& s, float logp, float& d)
 {
     const float w = s.w, a = s.a;
-    const float ratio = expf(logp - s.old_logp);
-    const float plain = ratio * a, clipped = fminf(fmaxf(ratio, p.low), p.high) * a;
+    const float change = logp - s.old_logp, ratio = expf(change);
+    float plain = ratio * a;
+    const float clipped = fminf(fmaxf(ratio, p.low), p.high) * a;
+    if (ratio == INFINITY) { // the product may be a number of binary32 all the same, as 0 is for an advantage of 0
+        const float half = expf(0.5f * change);
+        plain = half * a * half;
+    }
     const bool active = !(plain > clipped); // also where one is NaN, which then shows
     const float term = active ? -plain : -clipped;
     float kl = 0.0f, penalty = 0.0f;

@@ -104,3 +104,46 @@ def test_sequences_of_probability_zero(dq, lens, vocab, own_stream):
                 d[start[k]:start[k + 1]] = 0.5 * g / pairs
             grad, bound = ref.dlogits(sm, d, d_err=err.expand(rows) * 0.25 + 4 * U)
             ref.close(out, grad, torch.nan_to_num(bound))
+
+
+def policy_rows(dq, logp_minus_old, adv, ref_minus_logp=None, beta=0.0, at_zero=(), vocab=90, dtype=torch.float32, rows=None):
+    """One policy loss whose rows have the given differences; rows in at_zero take a token of probability 0.  -> sums, logp, dlogits, and what they are of"""
+    n = len(adv)
+    z, y, gen = make_logits(n, vocab, dtype, 17)
+    for r in at_zero:
+        z[r, y[r]] = -math.inf
+    sm = ref.softmax(z, y)
+    logp32 = torch.nan_to_num(sm["logp"], neginf=0.0)
+    old = (logp32 - torch.tensor(logp_minus_old, dtype=torch.float64)).float()
+    reference = None if ref_minus_logp is None else (logp32 + torch.tensor(ref_minus_logp, dtype=torch.float64)).float()
+    a, w = torch.tensor(adv, dtype=torch.float32), torch.full((n,), 1.0 / n)
+    loss, logp, out = torch.empty(4, device="cuda"), torch.empty(n, device="cuda"), torch.empty_like(z).cuda()
+    ws = torch.empty(dq.policy_loss_workspace_bytes(n, vocab), dtype=torch.uint8, device="cuda")
+    alone, ignored = torch.empty(4, device="cuda"), torch.empty(n, device="cuda")
+    up = lambda t: None if t is None else t.cuda()  # noqa: E731
+    for gradient, l, lp in ((out, loss, logp), (None, alone, ignored)):
+        dq.policy_loss(z.cuda(), y.cuda(), old.cuda(), a.cuda(), w.cuda(), l, lp, gradient, ws, ref_logp=up(reference), clip_low=0.2, clip_high=0.3, beta=beta)
+    torch.cuda.synchronize()
+    return loss, alone, logp, out, (sm, old, reference, a, w, z, y)
+
+
+@pytest.mark.parametrize("vocab", [5, 90, 3000, 9000, 70000])
+def test_ratios_beyond_binary32(dq, vocab):
+    """exp(logp - old_logp) beyond binary32 where its product with the advantage is not: 0 for an advantage of 0, 1e33 for one of -1e-10; a positive advantage is clipped."""
+    loss, alone, logp, out, (sm, old, _, a, w, z, y) = policy_rows(dq, [100.0, 100.0, 100.0, 0.1, 120.0, -200.0], [0.0, -1e-10, 2.0, 1.0, -1e-30, 1.0], vocab=vocab)
+    sums, d, sum_err, d_err, lp = ref.policy(sm, old, None, a, w, 0.2, 0.3, 0.0)
+    assert sums.isfinite().all() and float(sums[1]) > 1e32
+    # where the exponential overflows it is the square of one of half the exponent, whose error is twice one's
+    for l in (loss, alone):
+        ref.close(l, sums, 2 * sum_err)
+    ref.close(logp, lp, sm["logp_err"])
+    want, bound = ref.dlogits(sm, d, d_err=2 * d_err)
+    ref.close(out, want, bound)
+    assert not out[0].any() and not out[2].any()
+    # an advantage of 0 beside ordinary rows
+    loss, alone, logp, out, (sm, old, _, a, w, z, y) = policy_rows(dq, [95.0, 0.1, -0.1], [0.0, 1.0, -0.5], vocab=vocab)
+    sums, d, sum_err, d_err, lp = ref.policy(sm, old, None, a, w, 0.2, 0.3, 0.0)
+    for l in (loss, alone):
+        ref.close(l, sums, sum_err)
+    want, bound = ref.dlogits(sm, d, d_err=d_err)
+    ref.close(out, want, bound)
