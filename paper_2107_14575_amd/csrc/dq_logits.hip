@@ -394,7 +394,7 @@ __device__ __forceinline__ float4 policy_row(const policy_args& p, const policy_
     d = active ? -plain : 0.0f;
     if (p.ref_logp) {
         const float u = s.ref_logp - logp, e = expm1f(u);
-        kl = e - u;
+        kl = e == INFINITY ? e : e - u; // of a token of probability 0 infinite, not NaN
         if (p.beta != 0.0f) { // a divergence that is only looked at may be infinite
             penalty = p.beta * kl;
             d -= p.beta * e;

@@ -147,3 +147,23 @@ def test_ratios_beyond_binary32(dq, vocab):
         ref.close(l, sums, sum_err)
     want, bound = ref.dlogits(sm, d, d_err=d_err)
     ref.close(out, want, bound)
+
+
+@pytest.mark.parametrize("vocab", [5, 90, 3000, 9000, 70000])
+def test_divergence_of_a_token_of_probability_zero(dq, vocab):
+    """exp(u) - 1 - u is infinite for an infinite u of either sign, not NaN: with beta = 0 in its own sum alone, otherwise in the loss as well."""
+    for ref_minus in (0.5, -math.inf):
+        zero = (1,) if ref_minus == 0.5 else ()
+        for beta in (0.0, 0.1):
+            loss, alone, logp, out, (sm, old, reference, a, w, z, y) = policy_rows(dq, [0.1, 0.0, -0.1], [1.0, 0.5, -1.0], [0.2, ref_minus, -0.3], beta=beta, at_zero=zero, vocab=vocab)
+            assert float(loss[2]) == math.inf and float(alone[2]) == math.inf
+            assert (float(logp[1]) == -math.inf) == bool(zero) and logp[[0, 2]].isfinite().all()
+            assert out[[0, 2]].isfinite().all()
+            if beta:
+                assert float(loss[0]) == math.inf and float(alone[0]) == math.inf
+            else:
+                plain = ref.policy(sm, old, None, a, w, 0.2, 0.3, 0.0)
+                bound = torch.nan_to_num(plain[2], nan=4e-6, posinf=4e-6)
+                for l in (loss, alone):
+                    ref.close(l[:2], plain[0][:2], bound[:2])
+                assert out.isfinite().all()
