@@ -643,12 +643,15 @@ struct tensor_list {
     {
         taker& a = c.a;
         PyObject* list = a.object();
-        PyObject* items = a.ok ? PySequence_Fast(list, "a list of tensors is wanted") : nullptr;
+        PyObject* sequence = a.ok ? PySequence_Fast(list, "a list of tensors is wanted") : nullptr;
+        // a tuple, which holds its tensors: their methods may be any code, and the list could change
+        PyObject* items = sequence ? PySequence_Tuple(sequence) : nullptr;
+        Py_XDECREF(sequence);
         if (!items) {
             a.ok = false;
             return;
         }
-        const Py_ssize_t n = PySequence_Fast_GET_SIZE(items);
+        const Py_ssize_t n = PyTuple_GET_SIZE(items);
         try {
             data.reserve(n);
             len.reserve(n);
@@ -659,7 +662,7 @@ struct tensor_list {
         }
         if (n > INT32_MAX) c.refuse(name, "too many tensors");
         for (Py_ssize_t i = 0; i < n && a.ok; ++i) {
-            PyObject* t = PySequence_Fast_GET_ITEM(items, i);
+            PyObject* t = PyTuple_GET_ITEM(items, i);
             const int kind = c.kind(t);
             if (a.ok && kind > DQ_BF16) c.refuse(name, "float32, float16 or bfloat16 is wanted");
             if (a.ok && !c.truth(t, a.lib->is_contiguous)) c.refuse(name, "not contiguous");
