@@ -112,6 +112,19 @@ __global__ __launch_bounds__(THREADS) void k_squares(clip_table t, double* __res
 }
 
 __device__ __forceinline__ double clip_factor(double norm, double max_norm) { return norm <= max_norm ? 1.0 : max_norm / norm; }
+// The factor as binary32 holds it, f = first * second: where it is below the normal numbers its products with a gradient that has grown so far are not, and
+// `second` is the power of two that keeps `first` among them.  What that rounds in x * second is below the last place of the product.  Otherwise `second`
+// is 1, whose product changes nothing.
+struct clip_scale {
+    float first, second;
+    __device__ __forceinline__ explicit clip_scale(double f)
+    {
+        const double small = f < 0x1p-252 ? 0x1p-149 : f < 0x1p-126 ? 0x1p-126 : 1.0; // 1 for NaN
+        first = static_cast<float>(f / small);
+        second = static_cast<float>(small);
+    }
+    __device__ __forceinline__ float operator*(float x) const { return x * second * first; }
+};
 
 __device__ __forceinline__ double total_norm(const double* __restrict__ partials, int n)
 {
@@ -129,7 +142,7 @@ __global__ __launch_bounds__(THREADS) void k_total(const double* __restrict__ pa
 // One thread's share of the pieces times f, `back` pieces from the last one and `step` more each time: as the caches hold them.  ROW: into binary32, a tensor's
 // first piece with the pads behind it.
 template <bool ROW>
-__device__ __forceinline__ void scale_pieces(const clip_table& t, float f, uint32_t back, uint32_t step, int tid)
+__device__ __forceinline__ void scale_pieces(const clip_table& t, const clip_scale& f, uint32_t back, uint32_t step, int tid)
 {
     for (; back < t.pieces; back += step) {
         const clip_piece p = piece_of(t, t.pieces - 1 - back);
@@ -137,9 +150,9 @@ __device__ __forceinline__ void scale_pieces(const clip_table& t, float f, uint3
             using T = std::remove_cv_t<std::remove_pointer_t<decltype(g)>>;
             using Out = std::conditional_t<ROW, float, T>;
             Out* out = static_cast<Out*>(t.dst[p.tensor]);
-            if (!ROW && f == 1.0f && static_cast<const void*>(out) == g) return;
+            if (!ROW && f.first == 1.0f && f.second == 1.0f && static_cast<const void*>(out) == g) return;
             const int64_t end = p.index == 0 ? parts.end_of(tid, p.len) : -1;
-            if (end >= 0) out[end] = static_cast<Out>(static_cast<float>(g[end]) * f);
+            if (end >= 0) out[end] = static_cast<Out>(f * static_cast<float>(g[end]));
             if (ROW && p.index == 0 && p.len + tid < (p.len + DQ_GRANULE - 1) / DQ_GRANULE * DQ_GRANULE) out[p.len + tid] = static_cast<Out>(0.0f);
             g += parts.head;
             out += parts.head;
@@ -156,7 +169,7 @@ __device__ __forceinline__ void scale_pieces(const clip_table& t, float f, uint3
                     if (first + i * THREADS < 2 * parts.vecs) {
                         float x[8];
                         unpack<T>(vec{ v[i][0], v[i][1], 0, 0 }, x);
-                        const float y[4] = { x[0] * f, x[1] * f, x[2] * f, x[3] * f };
+                        const float y[4] = { f * x[0], f * x[1], f * x[2], f * x[3] };
                         store_vec(out + (first + i * THREADS) * 4, pack<float>(y));
                     }
             } else {
@@ -169,7 +182,7 @@ __device__ __forceinline__ void scale_pieces(const clip_table& t, float f, uint3
                     if (first + i * THREADS < parts.vecs) {
                         float x[PER<T>];
                         unpack<T>(v[i], x);
-                        for (int j = 0; j < PER<T>; ++j) x[j] *= f;
+                        for (int j = 0; j < PER<T>; ++j) x[j] = f * x[j];
                         store_vec(out + (first + i * THREADS) * PER<T>, pack<Out>(x));
                     }
             }
@@ -182,7 +195,7 @@ __global__ __launch_bounds__(THREADS) void k_scale(clip_table t, const double* _
 {
     const double N = total_norm(partials, n_partials);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(N);
-    scale_pieces<ROW>(t, static_cast<float>(clip_factor(N, max_norm)), blockIdx.x, gridDim.x, threadIdx.x);
+    scale_pieces<ROW>(t, clip_scale(clip_factor(N, max_norm)), blockIdx.x, gridDim.x, threadIdx.x);
 }
 
 // Both passes by one workgroup, its four quarters a piece each at a time: few pieces are two launches' latency.
@@ -196,7 +209,7 @@ __global__ __launch_bounds__(FEW_THREADS) void k_clip_few(clip_table t, double m
     add_squares(mine, t, quarter, FEW_THREADS / THREADS, tid);
     const double N = sqrt(workgroup_sum<FEW_THREADS>(mine));
     if (threadIdx.x == 0) *norm = static_cast<float>(N);
-    scale_pieces<ROW>(t, static_cast<float>(clip_factor(N, max_norm)), quarter, FEW_THREADS / THREADS, tid);
+    scale_pieces<ROW>(t, clip_scale(clip_factor(N, max_norm)), quarter, FEW_THREADS / THREADS, tid);
 }
 
 // A worker's norms in the registers of one workgroup, HELD of each of its threads.
@@ -215,11 +228,11 @@ __global__ __launch_bounds__(HELD_THREADS) void k_clip_norms(const float* __rest
     for (int i = 0; i < HELD; ++i) mine = fma(static_cast<double>(v[i]), static_cast<double>(v[i]), mine);
     const double N = sqrt(workgroup_sum<HELD_THREADS>(mine));
     if (threadIdx.x == 0) total[blockIdx.x] = static_cast<float>(N);
-    const float f = static_cast<float>(clip_factor(N, max_norm));
+    const clip_scale f(clip_factor(N, max_norm));
 #pragma unroll
     for (int i = 0; i < HELD; ++i) {
         const int l = i * HELD_THREADS + threadIdx.x;
-        if (l < n_seg) out[row + l] = v[i] * f;
+        if (l < n_seg) out[row + l] = f * v[i];
     }
 }
 
@@ -255,12 +268,12 @@ __global__ __launch_bounds__(THREADS) void k_norm_scale(const float* __restrict_
 {
     const double N = total_norm(partials + blockIdx.y * shares, shares);
     if (blockIdx.x == 0 && threadIdx.x == 0) total[blockIdx.y] = static_cast<float>(N);
-    const float f = static_cast<float>(clip_factor(N, max_norm));
+    const clip_scale f(clip_factor(N, max_norm));
     const float* row = norms + static_cast<int64_t>(blockIdx.y) * n_seg;
     float* to = out + static_cast<int64_t>(blockIdx.y) * n_seg;
     const dq_parts<float, int64_t> parts(row, n_seg);
     const int64_t end = blockIdx.x == 0 ? parts.end_of(threadIdx.x, n_seg) : -1;
-    if (end >= 0) to[end] = row[end] * f;
+    if (end >= 0) to[end] = f * row[end];
     for (int64_t at = static_cast<int64_t>(blockIdx.x) * PIECE + threadIdx.x; at < parts.vecs; at += static_cast<int64_t>(shares) * PIECE) {
         vec v[AT_ONCE];
 #pragma unroll
@@ -269,7 +282,7 @@ __global__ __launch_bounds__(THREADS) void k_norm_scale(const float* __restrict_
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i)
             if (at + i * THREADS < parts.vecs) {
-                const float x[4] = { __uint_as_float(v[i][0]) * f, __uint_as_float(v[i][1]) * f, __uint_as_float(v[i][2]) * f, __uint_as_float(v[i][3]) * f };
+                const float x[4] = { f * __uint_as_float(v[i][0]), f * __uint_as_float(v[i][1]), f * __uint_as_float(v[i][2]), f * __uint_as_float(v[i][3]) };
                 store_vec(to + parts.head + (at + i * THREADS) * 4, pack<float>(x));
             }
     }
