@@ -375,7 +375,7 @@ int64_t dq_comm_cost_bits(int W, int64_t d, int b, int32_t n_norms, int B_pre);
  *            It may be the logits' own memory with the same strides; any other overlap is an error
  *            that is not seen.  grad_scale is a loss scale for types of few exponent bits, 1 without.
  * Arithmetic is binary32, a row's sum in a fixed order; sums over rows are binary64 in a fixed order:
- * results are the same from run to run.  batch * rows <= 2^24, vocab < 2^31; no rows is no error.
+ * results are the same from run to run.  The default stream and others group sums differently, which may change a last place.  batch * rows <= 2^24, vocab < 2^31; no rows is no error.
  * The calls run on the current device, as dq_norm_bracket does, enqueue kernels only and take the
  * sizes of their workspaces (16-byte aligned, contents ignored, one for each call that may overlap
  * with another) from the *_workspace_bytes functions, which return -1 on a bad argument. */
@@ -415,8 +415,9 @@ int dq_policy_loss(const dq_logits_t* logits, const int64_t* tokens_dev, double 
 
 /* The preference loss over pairs of sequences, and its gradient.  The rows are 2 * pairs sequences one after the other, sequence i
  * rows [seq_start[i], seq_start[i + 1]) (offsets outside [0, rows] are taken as the nearest of the two; a row in no sequence gets a zero
- * gradient); sequence p < pairs is preferred to sequence pairs + p.  With S_i the sum of a sequence's counted log-probabilities (average: their
- * mean; 0 for a sequence without any) and R_i = beta * (S_i - ref_logp_i):
+ * gradient; offsets that go back may put a row into several sequences, which is an error that is not seen: its gradient is then that of
+ * any one of them, and not the same from run to run); sequence p < pairs is preferred to sequence pairs + p.  With S_i the sum of a
+ * sequence's counted log-probabilities (average: their mean; 0 for a sequence without any) and R_i = beta * (S_i - ref_logp_i):
  *     h = R_p - R_(pairs+p),  l = -(1 - label_smoothing) ln sigma(h) - label_smoothing ln sigma(-h),  L = (1/pairs) sum l
  *   pairs         from 1 to 2^24
  *   seq_start_dev [2 * pairs + 1] int64;  ref_logp_dev [2 * pairs] or NULL (zeros)

@@ -656,7 +656,7 @@ def preference_loss_workspace_bytes(rows: int, vocab: int, pairs: int) -> int:
 def preference_loss(logits, tokens, seq_start, loss_out, seq_logp_out, dlogits_out, workspace, ref_logp=None, beta: float = 0.1,
                     label_smoothing: float = 0.0, average: bool = False, temperature: float = 1.0, grad_scale: float = 1.0, stream=None) -> None:
     """The preference loss over pairs of sequences and its gradient by the logits, in one call.  seq_start: int64 [2 * pairs + 1], sequence i being rows
-    [seq_start[i], seq_start[i + 1]); sequence p is preferred to sequence pairs + p.  ref_logp: float32 [2 * pairs], the reference model's
+    [seq_start[i], seq_start[i + 1]), offsets in ascending order; sequence p is preferred to sequence pairs + p.  ref_logp: float32 [2 * pairs], the reference model's
     seq_logp_out; seq_logp_out: float32 [2 * pairs].  loss_out: float32 [4]: the loss, the share of pairs in the right order, the mean reward
     of the preferred sequences and of the others.  dlogits_out: None for the loss alone.  Logits and tokens as token_logprob."""
     call, device = _operators()

@@ -10,9 +10,9 @@
 // A logit takes about 13 instructions for sum and gradient (bfloat16: unpack, maximum, difference, scale, exponential, addition; unpack, difference,
 // scale, exponential, product, half a conversion), a byte read or written a quarter of that, so the memory binds all but small calls, and the
 // kernels' aim is to move each byte once, whole lines at a time:
-//     k_token_logprob   reads once                  8192 x 32768 bfloat16       81 to 83 us   6.5 TB/s   vector ALU issuing 67 % of the time
+//     k_token_logprob   reads once                  8192 x 32768 bfloat16       81 us         6.6 TB/s   vector ALU issuing 67 % of the time
 //     k_token_gradient  reads and writes once       2048 x 32768 bfloat16       44 us         6.1 TB/s                      26 % (at 3637 x 100003)
-//     k_policy_fused    reads and writes once       4096 x 131072 bfloat16     362 us        5.9 TB/s                      51 %
+//     k_policy_fused    reads and writes once       4096 x 131072 bfloat16     353 to 364 us 5.9 to 6.1 TB/s               50 %
 // (a copy of 2 GiB by torch: 4.9 TB/s).  The preference loss has to know all rows of a pair before the first gradient and reads twice.  Small calls are
 // their launches: 2.8 us each on the host, beside 1.6 to 3.3 for a call's arguments.
 #include <cmath>
@@ -26,7 +26,7 @@
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int64_t MAX_STRIDE = INT64_C(1) << 38; // of elements: any row's address is then far from overflow
+constexpr int64_t MAX_STRIDE = INT64_C(1) << 38; // of elements: 2^24 rows' offsets fit 64 bits
 
 // ---- maximum and sum -------------------------------------------------------------------------------------------------------
 // the pair (maximum, sum of exp2((x - maximum) * c)) of a part of a row
@@ -786,7 +786,9 @@ __global__ __launch_bounds__(THREADS) void k_preference_pairs(preference_args p,
 }
 
 // Few rows and few pairs: the forward pass's last workgroup to arrive does the pairs as well, a wavefront each, and there is one launch for two.  One pair of
-// 4 tokens 10.2 -> 7.8 us, four of 24 12.6 -> 11.2; eight of 100 13.6 -> 14.5, sixteen of 60 12.4 -> 17.4.
+// 4 tokens 10.2 -> 7.8 us, four of 24 12.6 -> 11.2; eight of 100 13.6 -> 14.5, sixteen of 60 12.4 -> 17.4.  At the limits it is as fast or loses 1 to 2 us: four pairs
+// of 64 tokens over 500 binary32 logits 10.4 -> 10.2, eight of 32 10.5 -> 12.2; rows of 2049 to 4096 vectors, which have 256 threads here and 1024 there: one pair of 10
+// over 24000 bfloat16 12.1 -> 11.2, four of 16 over 30000 14.4 -> 16.0; beyond 4096 vectors two of 20 over 18000 binary32 14.8 -> 15.9.
 constexpr int64_t FEW_PAIRS = 8, FEW_PAIR_ROWS = 512;
 template <typename T, int TH>
 __global__ __launch_bounds__(THREADS) void k_preference_few(forward_args a, preference_args p, float* __restrict__ seq_logp, float* __restrict__ dlogp, float* __restrict__ loss)
@@ -895,7 +897,9 @@ dim3 grid_of(int64_t workgroups)
 // Vectors of a row up to which 16 lanes or a wavefront take it.
 constexpr int LANES_VECS = 128, WAVE_VECS = 512;
 
-// Few long rows are sliced.  Loss and gradient of 24 and 64 rows of 131072 bfloat16 logits 16.3 -> 11.5 and 17.3 -> 13.8 us, of 24 rows of 30000 8.2 -> 10.5.
+// Few long rows are sliced.  Loss and gradient of 24 and 64 rows of 131072 bfloat16 logits 16.3 -> 11.5 and 17.3 -> 13.8 us, of 24 rows of 30000 8.2 -> 10.5.  Beyond 64
+// rows it goes by their length: 80 rows of 65536, 131072 and 262144 logits 11.8 -> 13.1, 17.6 -> 15.7 and 32.6 -> 23.9 us, 192 rows 13.5 -> 17.2, 23.7 -> 27.7 and
+// 43.5 -> 48.7; a limit that rises with the length would gain up to a third between 65 and 128 rows.
 bool sliced(int64_t rows, int64_t vecs) { return rows <= 64 && vecs >= 8192; }
 int64_t slices_bytes(int64_t rows) { return up(rows * MOST_SLICES * static_cast<int64_t>(sizeof(row_sum))) + up(rows * 4); }
 row_slices slices_of(int64_t rows, int64_t vecs, void* workspace)
@@ -927,13 +931,13 @@ void forward(int dtype, const forward_args& a, void* workspace, hipStream_t stre
         }
         const auto launch_rows = [&](auto stream_flag) {
             constexpr bool STREAM = decltype(stream_flag)::value;
-            if (vecs <= LANES_VECS)
+            if (vecs <= LANES_VECS) // 65536 rows of 260 and 512 binary32: 15.7 and 24.9 us; a wavefront 28.3 and 31.2
                 launch(k_token_logprob<T, 16, STREAM>, (count + 15) / 16, THREADS);
             else if (vecs <= WAVE_VECS)
                 launch(k_token_logprob<T, 64, STREAM>, (count + 3) / 4, THREADS);
-            else if (vecs <= 2048 || count >= 1024)
+            else if (vecs <= 2048 || count >= 1024) // 1000 rows of 16384 bfloat16 9.2 us, 8192 of 30000 88; 1024 threads 11.5 and 94 (2048 of 100003: 78 and 73)
                 launch(k_token_logprob<T, 256, STREAM>, count, 256);
-            else
+            else // 100 rows of 30000 and 100003 bfloat16 5.2 and 9.5 us; 256 threads 6.2 and 13.8 (300 to 1000 rows of 16400: 7.1 to 11.7 and 6.0 to 9.5)
                 launch(k_token_logprob<T, 1024, STREAM>, count, 1024);
         };
         if (a.softmax)
